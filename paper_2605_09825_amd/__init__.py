@@ -492,18 +492,22 @@ def _vector(t, n: int):
     return t.data_ptr()
 
 
-def _gate(gate, shape, dtype):
+def _gate(call: str, gate, shape, dtype):
     if gate is None:
         return None, 0
     if gate.dim() == 1:
         return _vector(gate, shape[1]), 0
-    return _rows_of(gate, shape, dtype)
+    p, ld = _rows_of(gate, shape, dtype)
+    if ld == 0:  # one row broadcast over all: refused here as the calls refuse it of any other operand, since of a gate 0 means an fp32 vector to them
+        raise Mxfp4Error(call, ESHAPE)
+    return p, ld
 
 
 def mxfp4_residual_norm_fwd(x, o, cfg: NormCfg, gate=None, w_post=None, w_pre=None, x_out=None, h=None, rstd=None,
                             want_x_out: bool = True, want_h: bool = True, branch_dtype=None, stream=None):
     """x' = residual_scale x + branch_scale gate n(o) and h = norm(x').  x [rows][cols] bf16 or fp32; o (or None), a gate per row and
-    h share a type of their own (branch_dtype where there is no o: bf16 unless given); a gate [cols] and the weights are fp32.
+    h share a type of their own (branch_dtype where there is no o: bf16 unless given); a gate [cols] and the weights are fp32.  A gate per row has
+    rows of its own (one broadcast over them is refused: it is the gate [cols], in fp32).
     Returns (x_out, h, rstd); an output not wanted is None."""
     shape, x_type, codes = x.shape, x.dtype, _types()
     rows, cols = shape
@@ -519,9 +523,9 @@ def mxfp4_residual_norm_fwd(x, o, cfg: NormCfg, gate=None, w_post=None, w_pre=No
             rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
     assert rstd.is_cuda and rstd.dtype is _fp32 and rstd.shape == (2, rows) and rstd.is_contiguous()
     _check("mxfp4_residual_norm_fwd", lib().mxfp4_residual_norm_fwd(
-        *_rows_of(x, shape, x_type), *_rows_of(o, shape, branch), *_gate(gate, shape, branch), _vector(w_post, cols), _vector(w_pre, cols),
-        rows, cols, codes[x_type], codes[branch], ctypes.byref(cfg), *_rows_of(x_out, shape, x_type), *_rows_of(h, shape, branch),
-        rstd.data_ptr(), _stream_ptr(stream)))
+        *_rows_of(x, shape, x_type), *_rows_of(o, shape, branch), *_gate("mxfp4_residual_norm_fwd", gate, shape, branch),
+        _vector(w_post, cols), _vector(w_pre, cols), rows, cols, codes[x_type], codes[branch], ctypes.byref(cfg),
+        *_rows_of(x_out, shape, x_type), *_rows_of(h, shape, branch), rstd.data_ptr(), _stream_ptr(stream)))
     return x_out, h, rstd
 
 
@@ -547,9 +551,9 @@ def mxfp4_residual_norm_bwd(dx_out, dh, x_out, o, rstd, cfg: NormCfg, gate=None,
     assert gate is None or dgate is None or dgate.dim() == gate.dim()
     _check("mxfp4_residual_norm_bwd", lib().mxfp4_residual_norm_bwd(
         *_rows_of(dx_out, shape, x_type), *_rows_of(dh, shape, branch), *_rows_of(x_out, shape, x_type), *_rows_of(o, shape, branch),
-        *_gate(gate, shape, branch), _vector(w_post, cols), _vector(w_pre, cols), _ptr(rstd), rows, cols, codes[x_type], codes[branch],
-        ctypes.byref(cfg), *_rows_of(dx, shape, x_type), *_rows_of(do, shape, branch), *_gate(dgate, shape, branch),
-        _vector(dw_post, cols), _vector(dw_pre, cols), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+        *_gate("mxfp4_residual_norm_bwd", gate, shape, branch), _vector(w_post, cols), _vector(w_pre, cols), _ptr(rstd),
+        rows, cols, codes[x_type], codes[branch], ctypes.byref(cfg), *_rows_of(dx, shape, x_type), *_rows_of(do, shape, branch),
+        *_gate("mxfp4_residual_norm_bwd", dgate, shape, branch), _vector(dw_post, cols), _vector(dw_pre, cols), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
     return workspace
 
 

@@ -124,3 +124,46 @@ def test_orthogonalize_refusals_and_workspace(L):
     assert mx.mxfp4_orthogonalize_workspace_bytes(0, 1, 1) == 0 and mx.mxfp4_orthogonalize_workspace_bytes(1, 1, (1 << 20) + 1) == 0
     # X's first words twice, its second ones, three symmetric matrices, at 2 bytes
     assert mx.mxfp4_orthogonalize_workspace_bytes(1, 128, 256) >= 3 * 2 * 128 * 256 + 3 * 2 * 128 * 128
+
+
+class Device:
+    """What the binding asks of a tensor before it hands its address on, of one that is in CUDA memory by its word alone."""
+    is_cuda = True
+
+    def __init__(self, t):
+        self.t, self.dtype, self.shape = t, t.dtype, t.shape
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def data_ptr(self):
+        return P
+
+
+@pytest.mark.parametrize("branch", ["bfloat16", "float32"])
+@pytest.mark.parametrize("what", ["forward", "backward", "dgate"])
+def test_a_gate_per_row_that_is_broadcast_over_rows_is_refused(L, monkeypatch, what, branch):
+    """Its leading dimension is 0, which the C calls take as one fp32 vector [cols] for all rows: refused with the code of any other operand's 0."""
+    import torch
+    monkeypatch.setattr(mx, "_stream_ptr", lambda stream: None)
+    branch = getattr(torch, branch)
+    dense = Device(torch.empty((4, 64), dtype=branch))
+    broadcast = Device(torch.empty(64, dtype=branch).expand(4, 64))
+    rstd, ws = Device(torch.empty((2, 4))), Device(torch.empty(1 << 20, dtype=torch.uint8))
+    cfg = mx.make_norm_cfg()
+    reached = []
+    for call in ("mxfp4_residual_norm_fwd", "mxfp4_residual_norm_bwd"):
+        monkeypatch.setattr(L, call, lambda *args: reached.append(args) or mx.OK)
+    with pytest.raises(mx.Mxfp4Error) as e:
+        if what == "forward":
+            mx.mxfp4_residual_norm_fwd(dense, dense, cfg, gate=broadcast, x_out=dense, h=dense, rstd=rstd)
+        else:
+            gate, dgate = (broadcast, dense) if what == "backward" else (dense, broadcast)
+            mx.mxfp4_residual_norm_bwd(dense, dense, dense, dense, rstd, cfg, gate=gate, dgate=dgate, dx=dense, workspace=ws)
+    assert e.value.status == mx.ESHAPE and not reached
+    # one row, or rows of their own, are the C call's to check
+    for rows in (1, 4):
+        t, r = Device(torch.empty((rows, 64), dtype=branch)), Device(torch.empty((2, rows)))
+        gate = Device(torch.empty(64, dtype=branch).expand(1, 64)) if rows == 1 else t
+        mx.mxfp4_residual_norm_fwd(t, t, cfg, gate=gate, x_out=t, h=t, rstd=r)
+        assert reached.pop()[5] == 64

@@ -461,6 +461,7 @@ typedef struct {
                           1.9, or those of b X X^T + c (X X^T)^2 beyond 15, over the steps                              */
     float eps;         /* added to the norm, > 0                                                                       */
     float out_scale;   /* of the output: sqrt(max(1, N / K)) or 0.2 sqrt(max(N, K)), for instance                       */
+    int32_t join_steps; /* 0: one step after the other.  1: two and three of them in one where that is faster, at a lower accuracy (below) */
 } mxfp4_muon_cfg;
 
 /*
@@ -470,9 +471,15 @@ typedef struct {
  * For each of `batch` matrices [N][K] of one shape (the layout of mxfp4_linear_bwd's dW):
  *   g         fp32 or bf16 (g_dtype: mxfp4_out), rows ld_g elements apart, matrices g_matrix
  *   momentum  fp32 [batch][N][K], dense, read and written; NULL: none
- *   out       bf16, rows ld_out elements apart, matrices out_matrix.  The products are of fp16 operands with fp32 sums, X and the diagonals
- *             are carried more exactly: the result is within about 1e-3 of the formula's before it is rounded to bf16.
+ *   out       bf16, rows ld_out elements apart, matrices out_matrix
  *   workspace mxfp4_orthogonalize_workspace_bytes(batch, N, K) bytes, 256-byte aligned; nothing in it is kept between calls
+ * Accuracy, as the root of the sum of squares of what is off, relative to the result's, before the rounding to bf16 (1.7e-3 by itself).  The products are of fp16
+ * operands with fp32 sums; X and the diagonals are carried more exactly.
+ *   Up to five steps with the usual coefficients (3.4445, -4.775, 2.0315): within 1e-3 of the formula's where N and K are 512 or more; 2e-3 from 200 on, 6e-3 from 64 on,
+ *   1.5e-2 below, the most where one direction holds nearly all of the gradient.  With join_steps: 5e-3.
+ *   That bounds the whole matrix.  A single direction can be off by more: one in which rows that hold all of the gradient differ by 1e-3 of themselves, by a tenth of itself.
+ *   Directions below about 1e-5 of |U| are not told from rounding.  Five steps leave them small; more steps bring them up, and the rounding with them.  Singular values
+ *   down to 1/N: 2e-3 after ten steps, 4e-3 after twenty; to 1/N^2: 7e-3, 2e-2; half of them below 1e-5 of the largest: 5e-3 after seven, 0.1 after ten (32-bit products: 2e-3).
  * A matrix of zeros gives zeros; one with an infinity or a NaN gives NaN.  The same inputs give the same bits.  N, K up to 2^20; batch == 0,
  * N == 0 or K == 0 is a valid empty call.
  */

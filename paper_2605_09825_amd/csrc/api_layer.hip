@@ -72,7 +72,7 @@ NormArgs norm_args(const mxfp4_norm_cfg *cfg, int64_t rows, int64_t cols, int x_
 
 // Whether the singular values of X stay in range: those of the first X are at most 1, and every step takes [0, most] into the polynomial's range over it,
 // whose extremes lie at its ends or where its derivative a + 3 b t + 5 c t^2 (t = s^2) vanishes.  They have to stay below what the fp16 scales of X (and so
-// of its square A, and of P A) and of Q leave room for.  joined: whether those of the P of two and three steps, multiplied, do too.
+// of its square A, and of P A) and of Q leave room for.  joined: whether those of the P of two and three steps, multiplied, do too (else steps stay single also where joining is asked for).
 bool coefficients_in_range(const mxfp4_muon_cfg *cfg, bool &joined)
 {
     const double a = cfg->a, b = cfg->b, c = cfg->c;
@@ -243,7 +243,7 @@ int mxfp4_orthogonalize(const void *g, int64_t ld_g, int64_t g_matrix, float *mo
                         int64_t batch, int64_t N, int64_t K, int g_dtype, const mxfp4_muon_cfg *cfg, void *workspace,
                         size_t workspace_bytes, void *hip_stream)
 {
-    if (!cfg || !known_type(g_dtype) || !flag(cfg->nesterov) || cfg->steps < 1 || cfg->steps > 64) return MXFP4_EINVAL;
+    if (!cfg || !known_type(g_dtype) || !flag(cfg->nesterov) || !flag(cfg->join_steps) || cfg->steps < 1 || cfg->steps > 64) return MXFP4_EINVAL;
     if (!(cfg->eps > 0.0f) || !isfinite(cfg->eps) || !isfinite(cfg->momentum) || !isfinite(cfg->out_scale)) return MXFP4_EINVAL;
     bool joined = false;
     if (!coefficients_in_range(cfg, joined)) return MXFP4_EINVAL;
@@ -273,7 +273,7 @@ int mxfp4_orthogonalize(const void *g, int64_t ld_g, int64_t g_matrix, float *mo
     a.g_fp32 = g_dtype == MXFP4_OUT_FP32;
     a.nesterov = cfg->nesterov;
     a.steps = cfg->steps;
-    a.joined = joined;
+    a.joined = cfg->join_steps && joined;
     a.mu = cfg->momentum;
     a.a = cfg->a;
     a.b = cfg->b;

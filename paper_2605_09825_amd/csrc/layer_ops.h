@@ -55,7 +55,7 @@ struct OrthoArgs {
     void *out;         // bf16 [batch][N][ld_out]
     int64_t batch, N, K, ld_g, ld_out, g_matrix, out_matrix;  // ..._matrix: elements from one matrix to the next
     int g_fp32, nesterov, steps;
-    bool joined;       // the coefficients allow two and three steps in one
+    bool joined;       // two and three steps in one: asked for, and within what the coefficients allow
     float mu, a, b, c, eps, out_scale;
     uint8_t *workspace;
 };

@@ -3,22 +3,23 @@
 //     `steps` times:  A = X X^T,  Q = b A + c A A,  X = P X with P = a I + Q
 // X is taken with fewer rows than columns (m <= n), so that A and Q are the small ones: G^T is worked on where G has more rows.
 //
-// Two and three steps in one.  The matrix of the next step is known without its X: A' = P A P, and X'' = P' P X.  That takes three more products of
-// m x m matrices (B = a A + A Q, A' = a B + Q B, T = P' P) and saves a product with X, its X X^T, and X's way to memory and back.  All m x m matrices
+// Two and three steps in one, on request.  The matrix of the next step is known without its X: A' = P A P, and X'' = P' P X.  That takes three more products
+// of m x m matrices (B = a A + A Q, A' = a B + Q B, T = P' P) and saves a product with X, its X X^T, and X's way to memory and back.  All m x m matrices
 // are polynomials in A: symmetric, and half of each product is enough.  So five steps, taken as three and two, take 2 x 3 m^2 n + 14 m^3 operations, as single
-// ones 5 x 3 m^2 n + 5 m^3: they are joined where X is so much wider than tall that this pays (joined_steps_pay).  Longer runs would lose A's small
-// eigenvalues, from which the steps bring a direction up, in the rounding of its large ones (each step multiplies them by a^2; X X^T of the X that is
-// really there does not drift).  Three only at the start, where the trace of A is 1: its rounding is 1.6e-4 / sqrt(m) at most there, against each eigenvalue
-// that still has to grow.  The last two steps are joined rather than two before the last: a step behind may double what they leave.
+// ones 5 x 3 m^2 n + 5 m^3: they are joined where X is so much wider than tall that this pays (joined_steps_pay).  A's small eigenvalues, from which the
+// steps bring a direction up, lose accuracy in the rounding of its large ones (each step multiplies them by a^2; X X^T of the X that is really there does
+// not drift): two and three steps lose some of it, which is why a caller has to ask for them, and longer runs would lose most.  Three only at the start,
+// where the trace of A is 1: its rounding is 1.6e-4 / sqrt(m) at most there, against each eigenvalue that still has to grow.  The last two steps are joined
+// rather than two before the last: a step behind may double what they leave.
 //
 // Types.  The products are of fp16 operands with fp32 sums; every operand has a fixed power of two as its scale, chosen so that the largest
 // singular value that X may reach fits (checked on the host for the coefficients given) and fp16's 11 bits hold all the way down to elements 2^-28 of it.
 // What the polynomial carries from step to step is kept more exactly than that: X as two fp16 words (hi + lo / 2048, 22 bits), of which the product takes
 // the first and the term with P's diagonal both, and the diagonals of all m x m matrices apart in fp32 (the products see zeros there), where nearly all of a
-// nearly orthogonal matrix's A and Q is.  Relative error of the result with random and partly low-rank gradients: 3e-4 to 9e-4 in single steps, 3e-4 to
-// 9e-4 joined; with X rounded to fp16 in every step 1.2e-3 to 2.4e-3, and 2.4e-2 where a few directions hold nearly all of the gradient (1e-4 here:
-// the small directions, which each step multiplies by a, no longer drown in the rounding of the large ones); with bf16 1e-2.  The result is bf16 (1.7e-3
-// by itself).
+// nearly orthogonal matrix's A and Q is.  Relative error of the result before its rounding to bf16 (1.7e-3 by itself), five steps, 512 rows and more, singular
+// values 1 / i, 1 / i^2, exponential over nine decades, of noise, and of noise below sixteen directions or one: single steps 1e-4 to 9e-4, joined ones 3e-4 to
+// 4e-3 (1024 x 4096 with 1 / i^2: 1.3e-4 and 1.6e-3, noise 3.0e-4 and 2.6e-4).  With X rounded to fp16 in every step 1.2e-3 to 2.4e-3, and 2.4e-2 where a few
+// directions hold nearly all of the gradient: the small ones, which each step multiplies by a, drown in the rounding of the large ones.  With bf16 1e-2.
 //
 // Layout.  Rows and columns are padded with zeros to whole 64s in the workspace, which the products turn into zeros again; nothing in the products' loops is
 // ragged.  X X^T and the m x m products take two operands whose rows lie along the contraction; in P X the second one's columns do, and its
@@ -872,8 +873,8 @@ hipError_t product(ProductArgs &p, int64_t batch, hipStream_t st)
     return product<2, 2, 3, MODE>(p, batch, st);
 }
 
-// Joined steps lose accuracy where a matrix is small (a single eigenvalue's error is not lost among many; 3 x 5: up to 1.6e-2), and gain nothing
-// there: launches are what small matrices take.  Above, where the products with X that they save take longer than the three of m x m ones that each adds, and a
+// Joined steps, where they are asked for, lose most accuracy where a matrix is small (a single eigenvalue's error is not lost among many; 3 x 5: up to 1.6e-2), and
+// gain nothing there: launches are what small matrices take.  Above, where the products with X that they save take longer than the three of m x m ones that each adds, and a
 // launch.  Five steps, single, as one and two pairs, as three and two: 4096 x 14336 4104, 3112, 2663 us; 4096 x 6144 1959, 1796, 1747; 1440 x 4320 381, 332,
 // 314; 1024 x 4096 228, 215, 209; but 2048 x 3000 443, 452 and 1024 x 1536 163, 175.
 constexpr int64_t JOINED_FROM = 512;

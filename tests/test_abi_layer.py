@@ -167,3 +167,11 @@ def test_a_gate_per_row_that_is_broadcast_over_rows_is_refused(L, monkeypatch, w
         gate = Device(torch.empty(64, dtype=branch).expand(1, 64)) if rows == 1 else t
         mx.mxfp4_residual_norm_fwd(t, t, cfg, gate=gate, x_out=t, h=t, rstd=r)
         assert reached.pop()[5] == 64
+
+
+def test_steps_are_joined_on_request_only(L):
+    assert mx.make_muon_cfg().join_steps == 0 and mx.make_muon_cfg(join_steps=True).join_steps == 1
+    cfg = mx.make_muon_cfg()
+    for join, status in ((0, mx.OK), (1, mx.OK), (2, mx.EINVAL), (-1, mx.EINVAL)):
+        cfg.join_steps = join
+        assert L.mxfp4_orthogonalize(None, 200, 0, None, None, 200, 0, 0, 100, 200, 1, ctypes.byref(cfg), None, 0, None) == status, join

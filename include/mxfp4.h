@@ -435,7 +435,7 @@ typedef struct {
     int32_t scaling;           /* mxfp4_rope_scaling                                           */
 } mxfp4_rope_cfg;
 
-/* table fp32 [positions][rot_dim / 2][2]: cos and sin of position * frequency, worked out in 64 bits; 16-byte aligned. */
+/* table fp32 [positions][rot_dim / 2][2]: cos and sin of position * frequency, worked out in 64 bits; 16-byte aligned.  Up to 2^31 positions. */
 int mxfp4_rope_table(float *table, int64_t positions, int64_t rot_dim, const mxfp4_rope_cfg *cfg, void *hip_stream);
 
 /*

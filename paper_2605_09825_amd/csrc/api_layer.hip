@@ -14,12 +14,16 @@ bool known_type(int dtype) { return dtype == MXFP4_OUT_BF16 || dtype == MXFP4_OU
 size_t element(int dtype) { return dtype == MXFP4_OUT_FP32 ? 4 : 2; }
 bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 bool flag(int v) { return v == 0 || v == 1; }
-constexpr int64_t MOST = int64_t(1) << 40;  // rows, strides: their products stay far below 2^63
+constexpr int64_t MOST = int64_t(1) << 40;      // rows, tokens, strides
+constexpr int64_t FURTHEST = int64_t(1) << 58;  // elements from the first to the last of a tensor, along each of its axes: offsets in bytes stay below 2^63
+constexpr int64_t MOST_POSITIONS = int64_t(1) << 31;  // of a rotary table
+// whether the last of n things that lie `stride` elements apart is within that (n, stride >= 0)
+bool in_reach(int64_t n, int64_t stride) { return n < 2 || stride <= FURTHEST / (n - 1); }
 
 // a matrix that a call reads or writes: its rows do not overlap, its elements lie at multiples of their size
-int check_matrix(const void *p, int64_t ld, int64_t cols, int dtype)
+int check_matrix(const void *p, int64_t ld, int64_t rows, int64_t cols, int dtype)
 {
-    if (ld < cols || ld > MOST) return MXFP4_ESHAPE;
+    if (ld < cols || ld > MOST || !in_reach(rows, ld)) return MXFP4_ESHAPE;
     return aligned(p, element(dtype)) ? MXFP4_OK : MXFP4_EALIGN;
 }
 
@@ -39,19 +43,19 @@ struct Operand {
 };
 // those that are there
 template <int N>
-int check_matrices(const Operand (&list)[N], int64_t cols)
+int check_matrices(const Operand (&list)[N], int64_t rows, int64_t cols)
 {
     for (const Operand &m : list)
         if (m.p)
-            if (const int rc = check_matrix(m.p, m.ld, cols, m.dtype)) return rc;
+            if (const int rc = check_matrix(m.p, m.ld, rows, cols, m.dtype)) return rc;
     return MXFP4_OK;
 }
 
-int check_gate(const void *gate, int64_t ld_gate, int64_t cols, int branch_dtype)
+int check_gate(const void *gate, int64_t ld_gate, int64_t rows, int64_t cols, int branch_dtype)
 {
     if (!gate) return MXFP4_OK;
     if (ld_gate == 0) return aligned(gate, 4) ? MXFP4_OK : MXFP4_EALIGN;
-    return check_matrix(gate, ld_gate, cols, branch_dtype);
+    return check_matrix(gate, ld_gate, rows, cols, branch_dtype);
 }
 
 NormArgs norm_args(const mxfp4_norm_cfg *cfg, int64_t rows, int64_t cols, int x_dtype, int branch_dtype)
@@ -122,7 +126,7 @@ int mxfp4_residual_norm_fwd(const void *x, int64_t ld_x, const void *o, int64_t 
     if (w_pre && !h) return MXFP4_EINVAL;
     if (!x || (!x_out && !h)) return MXFP4_EINVAL;
     const Operand list[] = {{x, ld_x, x_dtype}, {o, ld_o, branch_dtype}, {x_out, ld_x_out, x_dtype}, {h, ld_h, branch_dtype}};
-    if ((rc = check_matrices(list, cols)) != MXFP4_OK || (rc = check_gate(gate, ld_gate, cols, branch_dtype)) != MXFP4_OK) return rc;
+    if ((rc = check_matrices(list, rows, cols)) != MXFP4_OK || (rc = check_gate(gate, ld_gate, rows, cols, branch_dtype)) != MXFP4_OK) return rc;
     if (!aligned(w_post, 4) || !aligned(w_pre, 4) || !aligned(rstd, 4)) return MXFP4_EALIGN;
     if (!device_ok()) return MXFP4_EDEVICE;
     NormArgs a = norm_args(cfg, rows, cols, x_dtype, branch_dtype);
@@ -163,8 +167,8 @@ int mxfp4_residual_norm_bwd(const void *dx_out, int64_t ld_dx_out, const void *d
         if (cfg->post_norm && (d_o || dw_post || dgate) && !rstd) return MXFP4_EINVAL;
         const Operand list[] = {{dx_out, ld_dx_out, x_dtype}, {dh, ld_dh, branch_dtype}, {x_out, ld_x_out, x_dtype},
                                 {o, ld_o, branch_dtype}, {dx, ld_dx, x_dtype}, {d_o, ld_do, branch_dtype}};
-        if ((rc = check_matrices(list, cols)) != MXFP4_OK || (rc = check_gate(gate, ld_gate, cols, branch_dtype)) != MXFP4_OK) return rc;
-        if (dgate && !vector_gate && (rc = check_matrix(dgate, ld_dgate, cols, branch_dtype)) != MXFP4_OK) return rc;
+        if ((rc = check_matrices(list, rows, cols)) != MXFP4_OK || (rc = check_gate(gate, ld_gate, rows, cols, branch_dtype)) != MXFP4_OK) return rc;
+        if (dgate && !vector_gate && (rc = check_matrix(dgate, ld_dgate, rows, cols, branch_dtype)) != MXFP4_OK) return rc;
         if (sums && !workspace) return MXFP4_EINVAL;
         if (sums && workspace_bytes < mxfp4_residual_norm_workspace_bytes(rows, cols)) return MXFP4_EWORKSPACE;
     }
@@ -199,7 +203,7 @@ int mxfp4_rope_table(float *table, int64_t positions, int64_t rot_dim, const mxf
         (!isfinite(cfg->low) || !isfinite(cfg->high) || !(cfg->low > 0.0) || !(cfg->high > cfg->low) || !isfinite(cfg->original_positions) ||
          !(cfg->original_positions > 0.0)))
         return MXFP4_EINVAL;
-    if (positions < 0 || positions > (int64_t(1) << 31) || rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > 65536) return MXFP4_ESHAPE;
+    if (positions < 0 || positions > MOST_POSITIONS || rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > 65536) return MXFP4_ESHAPE;
     if (positions == 0) return MXFP4_OK;
     if (!table) return MXFP4_EINVAL;
     if (!aligned(table, 16)) return MXFP4_EALIGN;
@@ -215,11 +219,14 @@ int mxfp4_rope(const void *x, int64_t x_token, int64_t x_head, void *out, int64_
 {
     if (!known_type(dtype) || !flag(inverse) || (layout != MXFP4_ROPE_HALF && layout != MXFP4_ROPE_PAIRS)) return MXFP4_EINVAL;
     if (tokens < 0 || heads < 0 || tokens > MOST || heads > (1 << 20) || head_dim < 2 || head_dim > 65536 || rot_dim < 2 || rot_dim % 2 != 0 ||
-        rot_dim > head_dim || table_positions < 0)
+        rot_dim > head_dim || table_positions < 0 || table_positions > MOST_POSITIONS)
         return MXFP4_ESHAPE;
     if (tokens == 0 || heads == 0) return MXFP4_OK;
     if (!x || !out || !table) return MXFP4_EINVAL;
     if (x_token < 0 || x_head < 0 || out_token < 0 || out_head < 0 || x_token > MOST || x_head > MOST || out_token > MOST || out_head > MOST)
+        return MXFP4_ESHAPE;
+    if (!in_reach(tokens, x_token) || !in_reach(tokens, out_token) || !in_reach(heads, x_head) || !in_reach(heads, out_head) ||
+        tokens > FURTHEST / (heads * head_dim))
         return MXFP4_ESHAPE;
     // heads of the output must not overlap: token by token, or head by head
     const bool by_token = (heads == 1 || out_head >= head_dim) && (tokens == 1 || out_token >= (heads - 1) * out_head + head_dim);
@@ -228,8 +235,10 @@ int mxfp4_rope(const void *x, int64_t x_token, int64_t x_head, void *out, int64_
     if (x == out && (x_token != out_token || x_head != out_head)) return MXFP4_EINVAL;
     if (!aligned(x, element(dtype)) || !aligned(out, element(dtype)) || !aligned(positions, 4) || !aligned(table, 16)) return MXFP4_EALIGN;
     if (!device_ok()) return MXFP4_EDEVICE;
+    // (further from the table than there are tokens none of them is in it; the sum of position and token stays in range)
+    const int64_t first = first_position < -2 * MOST ? -2 * MOST : first_position > 2 * MOST ? 2 * MOST : first_position;
     const RopeArgs a{x, out, x_token, x_head, out_token, out_head, tokens, (int)heads, (int)head_dim, (int)rot_dim,
-                     dtype == MXFP4_OUT_FP32, layout == MXFP4_ROPE_PAIRS, inverse, positions, first_position, table, table_positions};
+                     dtype == MXFP4_OUT_FP32, layout == MXFP4_ROPE_PAIRS, inverse, positions, first, table, table_positions};
     return launch_rope(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? MXFP4_OK : MXFP4_EDEVICE;
 }
 
@@ -251,7 +260,7 @@ int mxfp4_orthogonalize(const void *g, int64_t ld_g, int64_t g_matrix, float *mo
     if (batch == 0 || N == 0 || K == 0) return MXFP4_OK;
     if (!g || !out || !workspace) return MXFP4_EINVAL;
     int rc;
-    if ((rc = check_matrix(g, ld_g, K, g_dtype)) != MXFP4_OK || (rc = check_matrix(out, ld_out, K, MXFP4_OUT_BF16)) != MXFP4_OK) return rc;
+    if ((rc = check_matrix(g, ld_g, N, K, g_dtype)) != MXFP4_OK || (rc = check_matrix(out, ld_out, N, K, MXFP4_OUT_BF16)) != MXFP4_OK) return rc;
     if (batch > 1 && (g_matrix < 0 || g_matrix > MOST || out_matrix < (N - 1) * ld_out + K || out_matrix > MOST)) return MXFP4_ESHAPE;
     if (workspace_bytes < ortho_workspace_bytes(batch, N, K)) return MXFP4_EWORKSPACE;
     if (!aligned(workspace, 256) || !aligned(momentum, 4)) return MXFP4_EALIGN;

@@ -175,3 +175,24 @@ def test_steps_are_joined_on_request_only(L):
     for join, status in ((0, mx.OK), (1, mx.OK), (2, mx.EINVAL), (-1, mx.EINVAL)):
         cfg.join_steps = join
         assert L.mxfp4_orthogonalize(None, 200, 0, None, None, 200, 0, 0, 100, 200, 1, ctypes.byref(cfg), None, 0, None) == status, join
+
+
+def test_sizes_whose_products_pass_64_bits_are_refused(L):
+    """Strides that no allocation has: what is worked out of them on the host, and the kernels' offsets, would wrap around."""
+    rope = dict(x=P, xt=6144, xh=128, out=P + 4096, ot=5120, oh=128, tokens=4, heads=40, dim=128, rot=128, dtype=0, layout=0, inverse=0,
+                positions=None, first=0, table=P, n=100, stream=None)
+    for by in (dict(tokens=2**24 + 1, heads=2, ot=2**40, oh=128, dim=256, rot=256),          # (tokens - 1) ot is 2^64: heads that overlap
+               dict(tokens=2**24 + 1, ot=2**40), dict(tokens=2**24 + 1, xt=2**40),             # ... and that do not
+               dict(tokens=2**40, heads=2**20, dim=2**16, rot=2, ot=2**36, oh=2**16, xt=0),    # 2^76 elements
+               dict(n=2**31 + 1), dict(n=2**62)):
+        assert L.mxfp4_rope(*changed(rope, **by)) == mx.ESHAPE, by
+    cfg = mx.make_norm_cfg()
+    norm = dict(x=P, ld_x=64, o=P, ld_o=64, gate=None, ld_gate=0, w_post=None, w_pre=None, rows=2**24 + 1, cols=64, xt=0, bt=0, cfg=ctypes.byref(cfg),
+                x_out=P, ld_x_out=64, h=P, ld_h=64, rstd=None, stream=None)
+    for by in (dict(ld_x=2**40), dict(ld_o=2**40), dict(ld_x_out=2**40), dict(ld_h=2**40), dict(gate=P, ld_gate=2**40)):
+        assert L.mxfp4_residual_norm_fwd(*changed(norm, **by)) == mx.ESHAPE, by
+    norm = dict(dx_out=P, ld_dxo=64, dh=P, ld_dh=64, x_out=P, ld_x=64, o=P, ld_o=64, gate=P, ld_gate=64, w_post=None, w_pre=None, rstd=P, rows=2**24 + 1,
+                cols=64, xt=0, bt=0, cfg=ctypes.byref(cfg), dx=P, ld_dx=64, do=P, ld_do=64, dgate=P, ld_dgate=64, dw_post=None, dw_pre=None,
+                ws=None, n=0, stream=None)
+    for by in ("ld_dxo", "ld_dh", "ld_x", "ld_o", "ld_gate", "ld_dx", "ld_do", "ld_dgate"):
+        assert L.mxfp4_residual_norm_bwd(*changed(norm, **{by: 2**40})) == mx.ESHAPE, by

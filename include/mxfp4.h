@@ -442,8 +442,8 @@ int mxfp4_rope_table(float *table, int64_t positions, int64_t rot_dim, const mxf
  * Rotary positions: the pairs (u, v) of each head's first rot_dim elements become (u cos - v sin, v cos + u sin); the others are
  * copied.  inverse = 1 turns back, which is also the gradient.
  *   x, out   element d of head h of token t at t * token + h * head + d (strides in elements, >= 0), bf16 or fp32 (dtype: mxfp4_out).  Heads
- *            of out must not overlap.  out may be x with the same strides: query and key heads of a fused projection are turned in place by
- *            one call.
+ *            of out must not overlap.  out may be x with the same strides (those of an axis of one aside), and must not overlap it otherwise: query
+ *            and key heads of a fused projection are turned in place by one call.
  *   positions  int32 [tokens]; NULL: first_position + t.  A position outside 0 .. table_positions - 1 makes its token's turned elements NaN.
  *   table      of mxfp4_rope_table for rot_dim, 16-byte aligned
  * rot_dim even, 2 <= rot_dim <= head_dim <= 65536.  tokens == 0 or heads == 0 is a valid empty call.

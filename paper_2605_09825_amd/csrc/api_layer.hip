@@ -232,7 +232,7 @@ int mxfp4_rope(const void *x, int64_t x_token, int64_t x_head, void *out, int64_
     const bool by_token = (heads == 1 || out_head >= head_dim) && (tokens == 1 || out_token >= (heads - 1) * out_head + head_dim);
     const bool by_head = (tokens == 1 || out_token >= head_dim) && (heads == 1 || out_head >= (tokens - 1) * out_token + head_dim);
     if (!by_token && !by_head) return MXFP4_ESHAPE;
-    if (x == out && (x_token != out_token || x_head != out_head)) return MXFP4_EINVAL;
+    if (x == out && ((tokens > 1 && x_token != out_token) || (heads > 1 && x_head != out_head))) return MXFP4_EINVAL;
     if (!aligned(x, element(dtype)) || !aligned(out, element(dtype)) || !aligned(positions, 4) || !aligned(table, 16)) return MXFP4_EALIGN;
     if (!device_ok()) return MXFP4_EDEVICE;
     // (further from the table than there are tokens none of them is in it; the sum of position and token stays in range)

@@ -440,7 +440,8 @@ int mxfp4_rope_table(float *table, int64_t positions, int64_t rot_dim, const mxf
 
 /*
  * Rotary positions: the pairs (u, v) of each head's first rot_dim elements become (u cos - v sin, v cos + u sin); the others are
- * copied.  inverse = 1 turns back, which is also the gradient.
+ * copied.  inverse = 1 is the gradient: the same with -sin.  It turns back what was turned where the table's attention factor is 1; with another one both directions
+ * multiply by it (as a call and its gradient have to), so that there and back is its square.
  *   x, out   element d of head h of token t at t * token + h * head + d (strides in elements, >= 0), bf16 or fp32 (dtype: mxfp4_out).  Heads
  *            of out must not overlap.  out may be x with the same strides (those of an axis of one aside), and must not overlap it otherwise: query
  *            and key heads of a fused projection are turned in place by one call.

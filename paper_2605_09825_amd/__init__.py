@@ -575,7 +575,8 @@ def mxfp4_rope_table(positions: int, rot_dim: int, cfg: RopeCfg, table=None, dev
 def mxfp4_rope(x, table, positions=None, first_position: int = 0, rot_dim: Optional[int] = None, layout: int = ROPE_HALF,
                inverse: bool = False, out=None, stream=None):
     """Turns the first rot_dim elements (all that the table has, unless given) of the heads of x [tokens][heads][head_dim], any strides but a unit
-    inner one, by their tokens' positions (int32 [tokens], or first_position + t).  out may be x; allocated here unless passed in."""
+    inner one, by their tokens' positions (int32 [tokens], or first_position + t).  out may be x; allocated here unless passed in.  inverse: the gradient, which turns the
+    other way and multiplies by the table's attention factor as the forward call does."""
     shape, dtype, codes = x.shape, x.dtype, _types()
     tokens, heads, dim = shape
     known, pairs, two = table.shape

@@ -1,5 +1,6 @@
 // Rotary positions: pairs (u, v) of a head's first `rot` elements become (u cos - v sin, v cos + u sin), with the angle position * frequency
-// of the pair.  Pairs are elements i and i + rot / 2 ("half") or 2 i and 2 i + 1 ("pairs").  The gradient turns the other way (inverse).
+// of the pair.  Pairs are elements i and i + rot / 2 ("half") or 2 i and 2 i + 1 ("pairs").  The gradient turns the other way (inverse); an
+// attention factor, which the table holds with cos and sin, multiplies in both.
 //
 // Memory bound: each head is read and written once (8192 tokens x 40 heads of 128 in bf16 36 us, 172 MB at 4.7 TB/s; 4010 x 32 in 32 bits, half of each
 // head turned, 27 us at 4.9; 24 tokens 3.4).  cos and sin come from a table in fp32, one row per position, built once in 64 bits:

@@ -23,3 +23,17 @@ def test_rope_in_place_through_two_views_of_one_token_or_head(shape, layout):
         whole.copy_(near.flatten())
         mx.mxfp4_rope(x, table, layout=layout, out=out)
         assert torch.equal(whole.view(shape), want)
+
+
+@pytest.mark.parametrize("layout", [mx.ROPE_HALF, mx.ROPE_PAIRS])
+@pytest.mark.parametrize("factor", [0.0, 1.5])
+def test_rope_there_and_back_is_the_square_of_the_attention_factor(factor, layout):
+    """cos^2 + sin^2 of table values (2^-23 each) is within 2^-21 of the factor's square, and two turns of fp32 elements within 2^-21 of |u| + |v|."""
+    cfg = mx.make_rope_cfg(scaling=mx.ROPE_SCALE_YARN, factor=16.0, attention_factor=factor)
+    square = (factor or 0.1 * torch.tensor(16.0, dtype=torch.float64).log().item() + 1.0) ** 2
+    table = mx.mxfp4_rope_table(300, 64, cfg)
+    x = torch.randn((300, 2, 96), device="cuda")
+    back = mx.mxfp4_rope(mx.mxfp4_rope(x, table, layout=layout), table, layout=layout, inverse=True)
+    assert torch.equal(back[..., 64:], x[..., 64:])
+    pair = x[..., :64].view(300, 2, 2, 32).abs().sum(2).repeat(1, 1, 2) if layout == mx.ROPE_HALF else x[..., :64].view(300, 2, 32, 2).abs().sum(3).repeat_interleave(2, -1)
+    assert ((back[..., :64].double() - square * x[..., :64].double()).abs() <= square * 2.0 ** -20 * pair.double()).all()

@@ -481,8 +481,8 @@ typedef struct {
  *   That bounds the whole matrix.  A single direction can be off by more: one in which rows that hold all of the gradient differ by 1e-3 of themselves, by a tenth of itself.
  *   Directions below about 1e-5 of |U| are not told from rounding.  Five steps leave them small; more steps bring them up, and the rounding with them.  Singular values
  *   down to 1/N: 2e-3 after ten steps, 4e-3 after twenty; to 1/N^2: 7e-3, 2e-2; half of them below 1e-5 of the largest: 5e-3 after seven, 0.1 after ten (32-bit products: 2e-3).
- * A matrix of zeros gives zeros; one with an infinity or a NaN gives NaN.  The same inputs give the same bits.  N, K up to 2^20; batch == 0,
- * N == 0 or K == 0 is a valid empty call.
+ * A matrix of zeros gives zeros; one with an infinity or a NaN gives NaN.  The same inputs give the same bits.  N, K up to 2^20, fewer than 2^24
+ * tiles of 64 x 64 in the batch (at most 65535 matrices); batch == 0, N == 0 or K == 0 is a valid empty call.
  */
 int mxfp4_orthogonalize(const void *g, int64_t ld_g, int64_t g_matrix, float *momentum, void *out, int64_t ld_out, int64_t out_matrix,
                         int64_t batch, int64_t N, int64_t K, int g_dtype, const mxfp4_muon_cfg *cfg, void *workspace,

@@ -74,6 +74,12 @@ NormArgs norm_args(const mxfp4_norm_cfg *cfg, int64_t rows, int64_t cols, int x_
     return a;
 }
 
+// Sizes of an update that are not too large: a launch has one tile of at least 64 x 64 per workgroup, of 256 threads, and fewer than 2^32 threads.
+bool ortho_sizes(int64_t batch, int64_t N, int64_t K)
+{
+    return batch <= 65535 && N <= ORTHO_MAX && K <= ORTHO_MAX && batch * ((N + 63) / 64) * ((K + 63) / 64) < (int64_t(1) << 24);
+}
+
 // Whether the singular values of X stay in range: those of the first X are at most 1, and every step takes [0, most] into the polynomial's range over it,
 // whose extremes lie at its ends or where its derivative a + 3 b t + 5 c t^2 (t = s^2) vanishes.  They have to stay below what the fp16 scales of X (and so
 // of its square A, and of P A) and of Q leave room for.  joined: whether those of the P of two and three steps, multiplied, do too (else steps stay single also where joining is asked for).
@@ -244,7 +250,7 @@ int mxfp4_rope(const void *x, int64_t x_token, int64_t x_head, void *out, int64_
 
 size_t mxfp4_orthogonalize_workspace_bytes(int64_t batch, int64_t N, int64_t K)
 {
-    if (batch < 1 || N < 1 || K < 1 || batch > 65535 || N > ORTHO_MAX || K > ORTHO_MAX) return 0;
+    if (batch < 1 || N < 1 || K < 1 || !ortho_sizes(batch, N, K)) return 0;
     return ortho_workspace_bytes(batch, N, K);
 }
 
@@ -256,7 +262,7 @@ int mxfp4_orthogonalize(const void *g, int64_t ld_g, int64_t g_matrix, float *mo
     if (!(cfg->eps > 0.0f) || !isfinite(cfg->eps) || !isfinite(cfg->momentum) || !isfinite(cfg->out_scale)) return MXFP4_EINVAL;
     bool joined = false;
     if (!coefficients_in_range(cfg, joined)) return MXFP4_EINVAL;
-    if (batch < 0 || N < 0 || K < 0 || batch > 65535 || N > ORTHO_MAX || K > ORTHO_MAX) return MXFP4_ESHAPE;
+    if (batch < 0 || N < 0 || K < 0 || !ortho_sizes(batch, N, K)) return MXFP4_ESHAPE;
     if (batch == 0 || N == 0 || K == 0) return MXFP4_OK;
     if (!g || !out || !workspace) return MXFP4_EINVAL;
     int rc;
@@ -264,9 +270,6 @@ int mxfp4_orthogonalize(const void *g, int64_t ld_g, int64_t g_matrix, float *mo
     if (batch > 1 && (g_matrix < 0 || g_matrix > MOST || out_matrix < (N - 1) * ld_out + K || out_matrix > MOST)) return MXFP4_ESHAPE;
     if (workspace_bytes < ortho_workspace_bytes(batch, N, K)) return MXFP4_EWORKSPACE;
     if (!aligned(workspace, 256) || !aligned(momentum, 4)) return MXFP4_EALIGN;
-    // (the launches hold one tile per workgroup)
-    const int64_t blocks = ((N + 63) / 64) * ((K + 63) / 64);
-    if (blocks * batch >= (int64_t(1) << 24)) return MXFP4_ESHAPE;
     if (!device_ok()) return MXFP4_EDEVICE;
     OrthoArgs a{};
     a.g = g;

@@ -196,3 +196,14 @@ def test_sizes_whose_products_pass_64_bits_are_refused(L):
                 ws=None, n=0, stream=None)
     for by in ("ld_dxo", "ld_dh", "ld_x", "ld_o", "ld_gate", "ld_dx", "ld_do", "ld_dgate"):
         assert L.mxfp4_residual_norm_bwd(*changed(norm, **{by: 2**40})) == mx.ESHAPE, by
+
+
+def test_no_workspace_is_named_for_an_update_that_is_refused(L):
+    """Sizes within 2^20 each, whose tiles of 64 x 64 are too many for a launch."""
+    for batch, N, K, there in ((1, 1 << 18, 1 << 18, False), (1, (1 << 18) - 64, 1 << 18, True), (65535, 1 << 14, 1 << 14, False), (256, 1 << 14, 1 << 14, False),
+                               (255, 1 << 14, 1 << 14, True), (1, 1 << 20, 1 << 20, False)):
+        need = mx.mxfp4_orthogonalize_workspace_bytes(batch, N, K)
+        cfg = mx.make_muon_cfg()
+        args = [P, K, N * K, None, P, K, N * K, batch, N, K, 1, ctypes.byref(cfg), P, 0, None]  # (a workspace of 0 bytes: no call gets beyond the checks)
+        assert L.mxfp4_orthogonalize(*args) == (mx.EWORKSPACE if there else mx.ESHAPE), (batch, N, K)
+        assert (need > 0) == there, (batch, N, K)

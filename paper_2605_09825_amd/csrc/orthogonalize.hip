@@ -313,11 +313,7 @@ struct Tile {
     static constexpr int TURN = (STRIP >> 9) % 4 == 0 ? 7 : 3;                      // 16-byte chunks of a strip's row v are exchanged by v & TURN
     static constexpr int PITCH = 16 * NV * 2 + 16, SLICE = 16 * NU * PITCH;         // a wave's outputs turned, rows along v
     static constexpr int MOST = 4 * SLICE > 8 * DEPTH * STRIP ? 4 * SLICE : 8 * DEPTH * STRIP;
-    // The widest tile touches its lines one stage ahead of their loads: every workgroup a quarter of them, those that share a panel different ones, so that the
-    // first of them to load a line does not wait for memory (P X 4096 x 14336 432 -> 402 us, 8192 x 8192 789 -> 728, but 4096 x 4096 99 -> 101;
-    // the other tiles lose 1 to 20 %: they are bound by what a compute unit may have under way).
-    static constexpr bool TOUCH = NU == 8 && NV == 8;
-    static constexpr int TOUCHED_AT = NBUF * STAGE > MOST ? NBUF * STAGE : MOST, LDS = TOUCHED_AT + (TOUCH ? 1024 : 0);
+    static constexpr int LDS = NBUF * STAGE > MOST ? NBUF * STAGE : MOST;
     static_assert(LDS <= 163840 && DEPTH >= 1, "LDS of a compute unit");
 };
 
@@ -409,27 +405,9 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(const ProductArgs p)
         else
             dma16<(q - NU) * 1024>(lds_v + buf, voff[q], pv);
     };
-    // A wave touches 32 lines of the first operand's next but NBUF stage, or of the second one's: four bytes of each, to where nothing reads them.
-    uint32_t touch_off = 0;
-    const uint8_t *touch_at = wave < 2 ? pu + step_u : pv + 128;
-    if (T::TOUCH) {
-        const int line = ((lane & 31) * 2 + (wave & 1)) * 4 + ((bu + bv) & 3);  // of the operand's 256
-        if (!ALONG && wave < 2) {
-            const int u = line % (ROW / 128) * 64;
-            touch_off = line / (ROW / 128) * ld_u + (u < end_u - 8 - u0 ? u : end_u - 8 - u0) * 2;
-        } else {
-            const int last = wave < 2 ? end_u - 1 - u0 : end_v - 1 - v0;
-            touch_off = (line < last ? line : last) * (wave < 2 ? ld_u : ld_v);
-        }
-    }
-    const auto touch = [&]() __attribute__((always_inline)) {
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds0 + T::TOUCHED_AT + wave * 256), "v"(touch_off), "s"(touch_at)
-                     : "memory");
-    };
     const auto next_stage = [&]() __attribute__((always_inline)) {
         pu += step_u;
         pv += 128;
-        if (T::TOUCH) touch_at += wave < 2 ? step_u : 128;
     };
 
     const int wu = wave >> 1, wv = wave & 1;
@@ -498,9 +476,7 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(const ProductArgs p)
             constexpr int half = decltype(which)::value;
             if (half) {
                 // all of this stage is in registers, of every wave behind the barrier, and the next one has arrived
-                if (T::TOUCH && left < stages && left > NBUF)  // (behind its loads the stage before has touched)
-                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NBUF - 2) * T::LOADS + 1) : "memory");
-                else if (NBUF > 2 && left >= NBUF)
+                if (NBUF > 2 && left >= NBUF)
                     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NBUF - 2) * T::LOADS) : "memory");
                 else
                     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -520,7 +496,6 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(const ProductArgs p)
                 __builtin_amdgcn_sched_barrier(0);
             });
         });
-        if (T::TOUCH && left > NBUF + 1) touch();
         next_stage();
         cur = nxt;
     }

@@ -91,11 +91,10 @@ bool coefficients_in_range(const mxfp4_muon_cfg *cfg, bool &joined)
     for (int step = 0; step < cfg->steps; ++step) {
         double roots[4] = {most * most, 0.0, 0.0, 0.0};
         const double half = 1.5 * b, under = half * half - 5.0 * c * a;
-        if (c != 0.0 && under >= 0.0) {
-            roots[1] = (-half + sqrt(under)) / (5.0 * c);
-            roots[2] = (-half - sqrt(under)) / (5.0 * c);
-        } else if (c == 0.0 && b != 0.0) {
-            roots[1] = -a / (3.0 * b);
+        if (under >= 0.0) {  // (the form of the roots in which nothing cancels, however small c is)
+            const double q = -(half + copysign(sqrt(under), half));
+            if (c != 0.0) roots[1] = q / (5.0 * c);
+            if (q != 0.0) roots[2] = a / q;
         }
         if (c != 0.0) roots[3] = -b / (2.0 * c);  // where b t + c t^2 is extreme
         double next = 0.0, largest_q = 0.0;

@@ -513,8 +513,11 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(const ProductArgs p)
     auto &acc = either<MAY_SPLIT>(apart, sums);
     if (MAY_SPLIT && p.splits > 1) {
         // Every piece writes its sums past the caches (agent scope: the XCDs' L2s are not coherent), waits until they are there, and counts itself; the last one
-        // to do so reads them past the caches, adds them up in their order, and goes on.  Nobody waits for anybody.  (With release and acquire in place
-        // of the wait every piece writes back and empties its XCD's L2: 1024 x 4096 in three pieces 23 us instead of 17.)
+        // to do so reads them past the caches, adds them up in their order, and goes on.  Nobody waits for anybody.  Each word is coherent by itself, being an
+        // atomic of agent scope on both sides; that the sums come before the count is not the language's memory model but gfx950's: such a store (SC1) is done, and
+        // taken off vmcnt, when all XCDs can see it, every thread's are waited for in front of the barrier, and the count is behind that; the loads (SC1 too)
+        // are issued when the count has come back.  The asm's memory clobbers keep the compiler to that order.  (With release and acquire in place of the wait every
+        // piece writes back and empties its XCD's L2: 1024 x 4096 in three pieces 23 us where this took 17.)
         uint64_t *pieces = reinterpret_cast<uint64_t *>(p.partial) + ((int64_t)tile_of_all * p.splits * 256 + threadIdx.x) * 2;  // [16 x 16][tile][piece][thread][2]
         const int64_t next = 256 * 2;
 #pragma unroll
@@ -754,8 +757,8 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(const ProductArgs p)
 }
 
 // X X^T on the smallest tiles: a few tiles leave most compute units idle, so that the long contraction is cut into pieces, whose sums the last
-// one to finish adds up (us: tiles' chains as below; 1.5 for writing and counting, 0.2 for each piece that is read, 0.004 for each one written).  64 x
-// 14336: 67 us whole, 17 in 16 pieces; 300 x 5000 26 and 12 in eight; 512 x 4096 22 and 12 in four; 1024 x 4096 20 and 17 in three (44 in 16).
+// one to finish adds up (us: tiles' chains as below; 1.5 for writing and counting, 0.2 for each piece that is read, 0.004 for each one written).  In
+// calls, whole and in pieces: 64 x 14336 57 us and 20 in twelve; 300 x 5000 24 and 15 in eight; 512 x 4096 19 and 13 in four; 1024 x 4096 19 and 16 in three.
 struct Pieces {
     int splits;
     double us;
@@ -800,10 +803,12 @@ hipError_t product(ProductArgs &p, int64_t batch, hipStream_t st)
 
 // Tiles of a product: those with the lowest estimate.  A compute unit that R tiles fall to takes a tile's start and end (`fixed`) and `stage` for each of its
 // stages, one tile after the other where one fills it; small tiles share it, `per_cu` of them, and a single one is bound by the chain through its
-// stages (`alone`).  Measured (us, P X of m x n unless named): 4096 x 14336 256 x 256 tiles 400 to 420, 192 x 256 453, 192 x 192 499, 128 x 128 496; 4096 x
-// 6144 154 with 192 x 256, 181 with 192 x 192, 165 with 128 x 128; 1440 x 4320 27 with 128 x 128, 36 with 64 x 64; X X^T there 27 with 64 x 64, 44 with
-// 128 x 128, of 4096 x 6144 99 with 192 x 192; A A of 4096 75 with 192 x 192, 105 with 128 x 128, of 1024 7.7 with 64 x 64.
-// What bounds the loop: of P X 4096 x 6144 the matrix instructions alone take 117 us, with fragment reads 135, the loads alone 114: a compute
+// stages (`alone`).  Measured in calls (us, P X of m x n unless named): 4096 x 14336 256 x 256 and 192 x 256 tiles 460, 192 x 192 519, 128 x 128 487; 4096 x
+// 6144 183 with 192 x 256, 196 with 128 x 128, 211 with 192 x 192, 226 with 256 x 256; 4096 x 4096 129 with 256 x 256, 138 with 128 x 128; 1440 x 4320 28 with
+// 128 x 128, 38 with 64 x 64; X X^T there 28 with 64 x 64, 44 with 128 x 128, of 4096 x 6144 98 with 192 x 192, 149 with 128 x 128; A A of 4096 74 with
+// 192 x 192, 103 with 128 x 128, of 1024 8.2 with 64 x 64, 17 with 128 x 128.  The constants are fitted to kernels launched by themselves on the same operands over and
+// over, which take up to a quarter less; the tiles they choose are the fastest, or within 2 % of them, in calls too.
+// What bounds the loop: by itself P X of 4096 x 6144 takes 154 us, its matrix instructions alone 117, with fragment reads 135, its loads alone 114: a compute
 // unit gets 60 to 78 bytes a ns out of L2 here, whatever the tile, which is what small tiles are bound by.  A tile of 192 x 192 keeps LDS as busy as the
 // matrix unit (1125 of 1152 clocks a stage), one of 256 x 256 three quarters of that.
 struct Choice {
@@ -848,10 +853,10 @@ hipError_t product(ProductArgs &p, int64_t batch, hipStream_t st)
     return product<2, 2, 3, MODE>(p, batch, st);
 }
 
-// Joined steps, where they are asked for, lose most accuracy where a matrix is small (a single eigenvalue's error is not lost among many; 3 x 5: up to 1.6e-2), and
-// gain nothing there: launches are what small matrices take.  Above, where the products with X that they save take longer than the three of m x m ones that each adds, and a
-// launch.  Five steps, single, as one and two pairs, as three and two: 4096 x 14336 4104, 3112, 2663 us; 4096 x 6144 1959, 1796, 1747; 1440 x 4320 381, 332,
-// 314; 1024 x 4096 228, 215, 209; but 2048 x 3000 443, 452 and 1024 x 1536 163, 175.
+// Joined steps, where they are asked for, lose most accuracy where a matrix is small (a single eigenvalue's error is not lost among many; 3 x 5: up to 1.6e-2),
+// and gain nothing there: launches are what small matrices take.  Above, where the products with X that they save take longer than the three of m x m ones that
+// each adds, and a launch.  Five steps, single and as three and two (us): 4096 x 14336 4180 and 2745; 6144 x 4096 1974 and 1773; 4320 x 1440 375 and 324; 1024 x
+// 4096 226 and 209; 600 x 8000 228 and 186; but 2048 x 3000 459 and 473, 1024 x 1536 163 and 180, 512 x 2048 130 and 133.
 constexpr int64_t JOINED_FROM = 512;
 bool joined_steps_pay(const OrthoLayout &l, int64_t batch)
 {

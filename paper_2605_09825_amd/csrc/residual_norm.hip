@@ -337,7 +337,10 @@ hipError_t fwd(const NormArgs &a, hipStream_t st)
 }
 
 // Workgroups of the backward pass, and so rows of partial sums: few rows get a workgroup each, many are walked by a workgroup of 8 to 16 waves on each
-// compute unit (8192 x 4096: 512 workgroups of eight waves took 118 us, and wrote and read twice the partial sums).
+// compute unit (8192 x 4096: 512 workgroups of eight waves took 118 us, and wrote and read twice the partial sums).  Both launches together, a workgroup per row
+// against walked (us, bf16, one gate): 256 rows of 64 columns 8.9 / 12.7, of 1440 10.6 / 13.2, of 4096 14.4 / 15.2; 512 rows 9.7 / 13.0, 13.3 / 13.4, 20.2 / 16.8;
+// 1024 rows 11.4 / 12.4, 19.1 / 14.8, 28.6 / 19.4; 2048 rows 14.7 / 12.9, 27.8 / 18.7, 47.9 / 25.5.  One limit for all widths: rows of 4096 columns would change over at
+// about 300, rows of up to 512 columns at about 1000 (in between they lose 1 to 3 us).
 constexpr int64_t FEW_ROWS = 512, MANY_GROUPS = 256;
 
 template <typename X, typename O, int W, int NV>

@@ -207,3 +207,16 @@ def test_no_workspace_is_named_for_an_update_that_is_refused(L):
         args = [P, K, N * K, None, P, K, N * K, batch, N, K, 1, ctypes.byref(cfg), P, 0, None]  # (a workspace of 0 bytes: no call gets beyond the checks)
         assert L.mxfp4_orthogonalize(*args) == (mx.EWORKSPACE if there else mx.ESHAPE), (batch, N, K)
         assert (need > 0) == there, (batch, N, K)
+
+
+def test_range_of_coefficients_that_are_nearly_a_cubic(L):
+    """A third coefficient that is nothing beside the others changes nothing of where the polynomial's extremes lie."""
+    def call(**kw):
+        return L.mxfp4_orthogonalize(None, 1, 0, None, None, 1, 0, 0, 1, 1, 1, ctypes.byref(mx.make_muon_cfg(**kw)), None, 0, None)
+
+    for c in (0.0, 1e-7, 1e-12, 1e-20, -1e-20, 1e-38):
+        assert call(steps=2, a=3.4, b=-2.7, c=c) == mx.EINVAL, c  # 1.47 at s^2 = 0.42; from there -3.6
+        assert call(steps=1, a=3.4, b=-2.7, c=c) == mx.OK, c
+        assert call(steps=64, a=1.5, b=-0.5, c=c) == mx.OK, c
+    assert call(steps=64) == mx.OK and call(steps=3, a=0.0, b=1.0, c=0.0) == mx.OK and call(steps=64, a=1.0, b=0.0, c=0.0) == mx.OK
+    assert call(steps=1, a=0.0, b=0.0, c=0.0) == mx.OK

@@ -474,6 +474,15 @@ def _types():
 _type_codes = _fp32 = None
 
 
+def _empty(shape, dtype, device, stream):
+    """A tensor of the call's stream: the allocator keeps what the caller drops from other streams while that one works on it."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 # (On the host these calls take as long as a small one does on the GPU: what is asked of a tensor is asked once.)
 def _rows_of(t, shape, dtype):
     """(pointer, leading dimension) of a CUDA matrix of this shape with unit inner stride; (None, 0) for None."""
@@ -516,11 +525,11 @@ def mxfp4_residual_norm_fwd(x, o, cfg: NormCfg, gate=None, w_post=None, w_pre=No
         import torch
         branch = branch or torch.bfloat16
         if x_out is None and want_x_out:
-            x_out = torch.empty(shape, dtype=x_type, device=x.device)
+            x_out = _empty(shape, x_type, x.device, stream)
         if h is None and want_h:
-            h = torch.empty(shape, dtype=branch, device=x.device)
+            h = _empty(shape, branch, x.device, stream)
         if rstd is None:
-            rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+            rstd = _empty((2, rows), torch.float32, x.device, stream)
     assert rstd.is_cuda and rstd.dtype is _fp32 and rstd.shape == (2, rows) and rstd.is_contiguous()
     _check("mxfp4_residual_norm_fwd", lib().mxfp4_residual_norm_fwd(
         *_rows_of(x, shape, x_type), *_rows_of(o, shape, branch), *_gate("mxfp4_residual_norm_fwd", gate, shape, branch),
@@ -545,7 +554,7 @@ def mxfp4_residual_norm_bwd(dx_out, dh, x_out, o, rstd, cfg: NormCfg, gate=None,
     branch = x_type if branch is None else branch.dtype
     if workspace is None:
         import torch
-        workspace = torch.empty(mxfp4_residual_norm_workspace_bytes(rows, cols), dtype=torch.uint8, device=(dh if dx_out is None else dx_out).device)
+        workspace = _empty(mxfp4_residual_norm_workspace_bytes(rows, cols), torch.uint8, (dh if dx_out is None else dx_out).device, stream)
     if rstd is not None:
         assert rstd.is_cuda and rstd.dtype is _fp32 and rstd.shape == (2, rows) and rstd.is_contiguous()
     assert gate is None or dgate is None or dgate.dim() == gate.dim()
@@ -566,7 +575,7 @@ def mxfp4_rope_table(positions: int, rot_dim: int, cfg: RopeCfg, table=None, dev
     """cos and sin of positions 0 .. positions - 1: fp32 [positions][rot_dim / 2][2]."""
     import torch
     if table is None:
-        table = torch.empty((positions, rot_dim // 2, 2), dtype=torch.float32, device=device)
+        table = _empty((positions, rot_dim // 2, 2), torch.float32, device, stream)
     assert table.is_cuda and table.dtype == torch.float32 and tuple(table.shape) == (positions, rot_dim // 2, 2) and table.is_contiguous()
     _check("mxfp4_rope_table", lib().mxfp4_rope_table(_ptr(table), positions, rot_dim, ctypes.byref(cfg), _stream_ptr(stream)))
     return table
@@ -582,8 +591,7 @@ def mxfp4_rope(x, table, positions=None, first_position: int = 0, rot_dim: Optio
     known, pairs, two = table.shape
     rot = 2 * pairs if rot_dim is None else rot_dim
     if out is None:
-        import torch
-        out = torch.empty(shape, dtype=dtype, device=x.device)
+        out = _empty(shape, dtype, x.device, stream)
     x_token, x_head, x_inner = x.stride()
     out_token, out_head, out_inner = out.stride()
     assert x.is_cuda and out.is_cuda and out.dtype == dtype and out.shape == shape and x_inner == 1 and out_inner == 1
@@ -615,13 +623,13 @@ def mxfp4_orthogonalize(g, cfg: MuonCfg, momentum=None, out=None, workspace=None
     batch = g.shape[0] if g.dim() == 3 else 1
     N, K = g.shape[-2:]
     if out is None:
-        out = torch.empty(g.shape, dtype=torch.bfloat16, device=g.device)
+        out = _empty(g.shape, torch.bfloat16, g.device, stream)
     assert g.is_cuda and g.dim() in (2, 3) and out.is_cuda and out.shape == g.shape and out.dtype == torch.bfloat16
     assert g.numel() == 0 or K == 1 or (g.stride(-1) == 1 and out.stride(-1) == 1)
     if momentum is not None:
         assert momentum.is_cuda and momentum.dtype == torch.float32 and momentum.shape == g.shape and momentum.is_contiguous()
     if workspace is None:
-        workspace = torch.empty(mxfp4_orthogonalize_workspace_bytes(batch, N, K), dtype=torch.uint8, device=g.device)
+        workspace = _empty(mxfp4_orthogonalize_workspace_bytes(batch, N, K), torch.uint8, g.device, stream)
 
     def strides(t):
         return t.stride(-2) if N > 1 else max(K, t.stride(-2)), t.stride(0) if t.dim() == 3 and batch > 1 else 0

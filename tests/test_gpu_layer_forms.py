@@ -37,3 +37,25 @@ def test_rope_there_and_back_is_the_square_of_the_attention_factor(factor, layou
     assert torch.equal(back[..., 64:], x[..., 64:])
     pair = x[..., :64].view(300, 2, 2, 32).abs().sum(2).repeat(1, 1, 2) if layout == mx.ROPE_HALF else x[..., :64].view(300, 2, 32, 2).abs().sum(3).repeat_interleave(2, -1)
     assert ((back[..., :64].double() - square * x[..., :64].double()).abs() <= square * 2.0 ** -20 * pair.double()).all()
+
+
+def test_what_a_call_allocates_belongs_to_its_stream():
+    """Else the allocator would hand a workspace that the caller drops to the current stream's next tensor, while the call's stream still works on it."""
+    side = torch.cuda.Stream()
+    x, o = (torch.randn((600, 4096), device="cuda").bfloat16() for _ in range(2))
+    w, g = torch.ones(4096, device="cuda"), torch.randn((300, 4096), device="cuda")
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    side.wait_stream(torch.cuda.current_stream())
+    cfg = mx.make_norm_cfg()
+    x_out, h, rstd = mx.mxfp4_residual_norm_fwd(x, o, cfg, w_pre=w, stream=side)
+    made = [x_out, h, rstd, mx.mxfp4_residual_norm_bwd(x, o, x_out, o, rstd, cfg, w_pre=w, dx=dx, dw_pre=dw, stream=side)]
+    made += mx.mxfp4_orthogonalize(g, mx.make_muon_cfg(), stream=side)
+    table = mx.mxfp4_rope_table(1 << 15, 128, mx.make_rope_cfg(), stream=side)
+    made += [table, mx.mxfp4_rope(x.view(600, 32, 128), table, stream=side)]
+    side.synchronize()
+    segments = torch.cuda.memory_snapshot()
+    for t in made:
+        mine = [s for s in segments if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]]
+        assert len(mine) == 1 and mine[0]["stream"] == side.cuda_stream, t.shape
+    here = mx.mxfp4_orthogonalize(g, mx.make_muon_cfg())[0]
+    assert torch.equal(here, made[4])

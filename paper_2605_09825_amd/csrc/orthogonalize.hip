@@ -855,8 +855,8 @@ hipError_t product(ProductArgs &p, int64_t batch, hipStream_t st)
 
 // Joined steps, where they are asked for, lose most accuracy where a matrix is small (a single eigenvalue's error is not lost among many; 3 x 5: up to 1.6e-2),
 // and gain nothing there: launches are what small matrices take.  Above, where the products with X that they save take longer than the three of m x m ones that
-// each adds, and a launch.  Five steps, single and as three and two (us): 4096 x 14336 4180 and 2745; 6144 x 4096 1974 and 1773; 4320 x 1440 375 and 324; 1024 x
-// 4096 226 and 209; 600 x 8000 228 and 186; but 2048 x 3000 459 and 473, 1024 x 1536 163 and 180, 512 x 2048 130 and 133.
+// each adds, and a launch.  Five steps, single and as three and two (us): 4096 x 14336 4045 and 2665; 6144 x 4096 1900 and 1724; 4320 x 1440 364 and 319; 1024 x
+// 4096 223 and 209; 600 x 8000 226 and 185; but 2048 x 3000 459 and 473, 1024 x 1536 163 and 180, 512 x 2048 130 and 133.
 constexpr int64_t JOINED_FROM = 512;
 bool joined_steps_pay(const OrthoLayout &l, int64_t batch)
 {
